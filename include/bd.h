@@ -467,10 +467,9 @@ bd_status bd_kv_read(const bd_kv_cache* cache, void* k_dev, void* v_dev, int32_t
  *  that sees no key, or stands at a negative position, gives zeros.  Keys that a
  *  query does not see have no effect on it, whatever their codes.
  *  scale: factor of the scores, > 0; 0 takes 1 / sqrt(head_dim).  Scores, softmax
- *  and sums are held in float32 and rounded once to dtype; fp32 queries are used
- *  with all their bits, weights of bfloat16 calls with 11.  (Weights are held
- *  relative to the largest weight times its page's V scale: those of a page whose V
- *  scale times weight lies 2^22 below that lose bits, below 2^33 they are 0.)
+ *  and sums are held in float32 and rounded once to dtype; queries are used with
+ *  all their bits.  (A weight times its page's V scale is held to 2^-22 of itself
+ *  or 2^-33 of the row's largest, whichever is more.)
  *  max_rows: about the most rows a request has, 0 if unknown (chooses the kernel's
  *  form; results are right for any value).
  *  ws_dev, ws_bytes: workspace of bd_kv_attention_workspace bytes, 256-byte

@@ -12,12 +12,13 @@
 // them: a tile lies in one page, K's scale multiplies its scores and V's
 // exponent goes into the weights, w = 2^(t + E_v - r) for the score t in log2
 // units and a running reference r, next to p = 2^(t - m) for the sum l.  Both
-// references lag (they move when a tile exceeds them by 2^8, or w 2^15), so w
-// uses fp16's upper range and what falls below its subnormals is 2^-32 of the
-// largest weight.  bf16 queries: one plane each, w rounded to fp16 (2^-11, an
-// eighth of the output's own rounding).  fp32 queries: three bf16 planes (24
-// bits, exact) and w as an fp16 pair (22 bits).  The models' bf16 pairs: two and
-// two.  Sums are fp32.
+// references are whole numbers, so that what leads from one to another is an exact
+// power of two, and lag (they move when a tile exceeds them by 2^8, or w 2^15).
+// The products take w as two fp16 parts: 22 bits, or 2^-33 of the row's largest w
+// where that is more (one part, 11 bits, moved one bf16 output in thirty to its
+// neighbour, 8e-4 of the outputs' norm against 5e-5; 8 windows of 128 rows over
+// 8320 keys took 113 us and take 133).  Queries are one, two or three bf16 planes
+// (bf16, the models' pairs, fp32: exact).  Sums are fp32.
 //
 // What bounds it.  Single tokens read every code once: 48 requests of very unequal
 // lengths, 0.80 GB in 163 us, 4.9 TB/s (a copy moves 5.2).  With 100 queries or
@@ -36,9 +37,9 @@ namespace bd {
 constexpr int A_HELD = 256;        // requests whose rows and lengths are held in LDS
 
 template <int MODE> struct AttnMode;
-template <> struct AttnMode<KVQ_BF16> { typedef bf16_t T; static constexpr int NQ = 1, NP = 1; };
-template <> struct AttnMode<KVQ_F32> { typedef float T; static constexpr int NQ = 3, NP = 2; };
-template <> struct AttnMode<KVQ_PAIR> { typedef bf16_t T; static constexpr int NQ = 2, NP = 2; };
+template <> struct AttnMode<KVQ_BF16> { typedef bf16_t T; static constexpr int NQ = 1; };
+template <> struct AttnMode<KVQ_F32> { typedef float T; static constexpr int NQ = 3; };
+template <> struct AttnMode<KVQ_PAIR> { typedef bf16_t T; static constexpr int NQ = 2; };
 
 __device__ __forceinline__ floatx16_k zero16() {
   return floatx16_k{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -195,7 +196,7 @@ template <int HD, int MODE, int QW, int KW, int BT>
 __global__ __launch_bounds__(64 * QW * KW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
   typedef typename AttnMode<MODE>::T T;
-  constexpr int NQ = AttnMode<MODE>::NQ, NP = AttnMode<MODE>::NP, NY = HD / 32, NT = 64 * QW * KW, AQ = 32 * QW;
+  constexpr int NQ = AttnMode<MODE>::NQ, NY = HD / 32, NT = 64 * QW * KW, AQ = 32 * QW;
   constexpr int LPW = 2 * NY / QW;             // 1 KiB loads a wave issues for a tile
   constexpr int LPS = BT * (LPW + 2);          // loads of a stage, its scales among them
   constexpr int D = KW == 8 && HD == 128 ? 2 : 3;   // stages of the ring: 128 KB, else 96 KB at most
@@ -455,8 +456,8 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
 #pragma unroll
         for (int b = 0; b < BT; ++b) {
           const float t = fmaxf(tm[b], __shfl_xor(tm[b], 32));
-          mn = fmaxf(mn, t);
-          rn = fmaxf(rn, t + ev[b] - 9.f);
+          mn = fmaxf(mn, ceilf(t));
+          rn = fmaxf(rn, ceilf(t) + (ev[b] - 9.f));
         }
         const float al = __builtin_amdgcn_exp2f(mn == -INFINITY ? 0.f : m_run - mn);
         const float ao = __builtin_amdgcn_exp2f(rn == -INFINITY ? 0.f : r_run - rn);
@@ -467,58 +468,48 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
         for (int d = 0; d < NY; ++d) oacc[d] *= ao;
       }
       const float m_ref = m_run == -INFINITY ? 0.f : m_run, r_ref = r_run == -INFINITY ? 0.f : r_run;
-      float lf[BT], fe[BT];
-      bool near = NP == 1;
+      // Weights straight from the exponent, w = 2^(t + E_v - r), as two fp16 parts; the
+      // sum's terms are p = w 2^-lf, lf = E_v + m - r.  From lf = 100 on w 2^-100 stands for
+      // p (below 2^-85, where l is 1/2 at least).  Below lf = -60, of a page whose V scale is
+      // nothing beside the reference's, w is 0 in fp16: p is summed here and the key left out.
+      const float ahead = m_ref - r_ref;
+      bool far = false;
 #pragma unroll
-      for (int b = 0; b < BT; ++b) {
-        lf[b] = fminf(ev[b] + m_ref - r_ref, 100.f);
-        fe[b] = __builtin_amdgcn_exp2f(lf[b]);
-        near = near && fe[b] >= 2.f;
-      }
-      f16x8 pf[BT][2][NP];
-      // Weights straight from the exponent, w = 2^(t - m + log2 fe), and the sum from
-      // the rounded weights the products take (two-term dot products).  Where fe is
-      // small (a page whose V scale is 2^8 below what the reference comes from) or
-      // weights have two parts, the sum takes fp32 terms p = 2^(t - m).
-      if (NP == 1 && __all(near)) {
-#pragma unroll
-        for (int b = 0; b < BT; ++b) {
-          const float ref = m_ref - lf[b];
-          float ws = 0.f;
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              const float w0 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j], sc[b], -ref));
-              const float w1 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j + 1], sc[b], -ref));
-              const f16x2 hi = __builtin_convertvector((floatx2_k){w0, w1}, f16x2);
-              ws = __builtin_amdgcn_fdot2(hi, (f16x2){1, 1}, ws, false);
-              pf[b][x][0][j] = hi[0];
-              pf[b][x][0][j + 1] = hi[1];
-            }
-          l_part = fmaf(ws, __builtin_amdgcn_rcpf(fe[b]), l_part);
-        }
-      } else {
+      for (int b = 0; b < BT; ++b) far |= ev[b] + ahead < -60.f;
+      if (__any(far)) {
 #pragma unroll
         for (int b = 0; b < BT; ++b)
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+          for (int i = 0; i < 16; ++i) {
+            const bool out = ev[b] + ahead < -60.f;
+            l_part += out ? __builtin_amdgcn_exp2f(fmaf(a[b][i], sc[b], -m_ref)) : 0.f;
+            a[b][i] = out ? -INFINITY : a[b][i];
+          }
+      }
+      // (w - hi as a product with a number that the compiler does not know is one mixed
+      // instruction; as a difference it is a conversion more)
+      float minus1 = -1.f;
+      asm("" : "+s"(minus1));
+      f16x8 pf[BT][2][2];
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-              const float p0 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j], sc[b], -m_ref));
-              const float p1 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j + 1], sc[b], -m_ref));
-              l_part += p0;
-              l_part += p1;
-              const float w0 = p0 * fe[b], w1 = p1 * fe[b];
-              const f16x2 hi = __builtin_convertvector((floatx2_k){w0, w1}, f16x2);
-              pf[b][x][0][j] = hi[0];
-              pf[b][x][0][j + 1] = hi[1];
-              if constexpr (NP == 2) {
-                const f16x2 lo = __builtin_convertvector((floatx2_k){w0 - (float)hi[0], w1 - (float)hi[1]}, f16x2);
-                pf[b][x][1][j] = lo[0];
-                pf[b][x][1][j + 1] = lo[1];
-              }
-            }
+      for (int b = 0; b < BT; ++b) {
+        float ws = 0.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j], sc[b], ev[b] - r_ref));
+            const float w1 = __builtin_amdgcn_exp2f(fmaf(a[b][8 * x + j + 1], sc[b], ev[b] - r_ref));
+            ws += w0;
+            ws += w1;
+            const f16x2 hi = __builtin_convertvector((floatx2_k){w0, w1}, f16x2);
+            const f16x2 lo = __builtin_convertvector((floatx2_k){fmaf((float)hi[0], minus1, w0), fmaf((float)hi[1], minus1, w1)}, f16x2);
+            pf[b][x][0][j] = hi[0];
+            pf[b][x][0][j + 1] = hi[1];
+            pf[b][x][1][j] = lo[0];
+            pf[b][x][1][j + 1] = lo[1];
+          }
+        l_part = fmaf(ws, __builtin_amdgcn_exp2f(-fminf(fmaxf(ev[b] + ahead, -60.f), 100.f)), l_part);
       }
 #pragma unroll
       for (int b = 0; b < BT; ++b)
@@ -528,7 +519,7 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
           for (int d = 0; d < NY; ++d) {
             const f16x8 vf = fp8x8_f16(vb[b][d][2 * x], vb[b][d][2 * x + 1]);
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p)
+            for (int p = 1; p >= 0; --p)
               oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[b][x][p], oacc[d], 0, 0, 0);
           }
       if (part && __any(bad)) {

@@ -1,0 +1,75 @@
+"""The paged attention's numbers against float64: outputs that are off by their own rounding alone, scales at both ends
+of their range, and the query pairs that the models' decoding takes."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import kv as ok
+from tests.test_gpu_kv import DEV, U, Pool, attn_bound, bd_, dev, host, run_attention, starts
+
+pytestmark = pytest.mark.gpu
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).double().numpy()
+
+
+def computed_bound(ref, mag, big, hd, keys):
+    """attn_bound's error before the output's rounding, for bf16 calls as for fp32 ones: weights of two fp16 parts, 2^-21."""
+    return attn_bound(ref, mag, big, hd, keys, torch.float32)
+
+
+FORMS = [([1057], [1], 16, 4, 128, 32, 1, 0),                                       # eight waves a query group
+         ([1057], [1], 16, 16, 64, 32, 1, 0),
+         ([9000, 40], [1, 5], 16, 4, 128, 64, 1, 0),                                # keys cut into ranges
+         ([1440] * 3, [96] * 3, 16, 4, 128, 32, 32, 64),                            # two query groups, by the hint
+         ([700] * 3, [96] * 3, 8, 2, 64, 32, 32, 16),
+         ([1100, 640, 900, 400], [1000, 640, 900, 77], 16, 8, 128, 64, 32, 0),      # four
+         ([900, 1100], [900, 1100], 16, 16, 64, 32, 1, 0),
+         ([2500] * 2, [64] * 2, 16, 4, 128, 32, 64, 1000)]
+
+
+@pytest.mark.parametrize("i", range(len(FORMS)))
+def test_bf16_outputs_are_the_rounded_float64_ones(i):
+    """An output lies between the roundings of the float64 value less and plus what fp32 arithmetic is off by.
+
+    Weights of 11 bits move one output in thirty to the next bfloat16 value, 8e-4 of the outputs' norm.  Scores in fp32
+    (sums of hd terms: sqrt(hd) 2^-24 of a size of about 5, then 2^-22 of v_exp_f32) leave weights off by some 1e-6 and
+    an output by 3e-6 at most, each key's error its own: 2 * 3e-6 of a step of 2^-8 is a share of 1.5e-3 moved by 2^-7 of
+    themselves at most, sqrt(1.5e-3) 2^-7 = 3e-4 of the norm."""
+    lens, cnt, H, Hkv, hd, T, B, max_rows = FORMS[i]
+    pool = Pool(300 + i, sum(-(-x // T) for x in lens) + 2, Hkv, hd, T, spread=1)
+    table = pool.tables(lens)
+    got, ref, _ = run_attention(pool, lens, cnt, B, H, torch.bfloat16, seed=i, table=table, max_rows=max_rows)
+    q = np.random.default_rng([5, i]).standard_normal((sum(cnt), H, hd))
+    q = host(dev(q, torch.float32).to(torch.bfloat16))
+    again, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q, table, starts(cnt), np.array(lens) - cnt, lens, B)
+    assert (again == ref).all()
+    e = computed_bound(ref, mag, big, hd, max(lens))
+    assert ((got >= bf16(ref - e)) & (got <= bf16(ref + e))).all(), float(np.mean((got < bf16(ref - e)) | (got > bf16(ref + e))))
+    off = np.linalg.norm(got - bf16(ref)) / np.linalg.norm(ref)
+    print(f"form {i}: {off:.2e} of the norm, {np.mean(got != bf16(ref)):.2e} of the outputs")
+    assert off <= 3e-4
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_small_weights_of_pages_of_far_larger_values(dtype):
+    """Weights of 2^-105.5 times values of 2^10 beside weights of 1 times values of 2^-100: the first are 2^4.5 times the second,
+    whatever reference the weights are held against."""
+    hd, T = 64, 32
+    pool = Pool(340, 10, 1, hd, T)
+    pool.kc[:] = 0
+    pool.ks[:] = 1.0
+    pool.vs[:], pool.vs[9] = 2.0 ** -100, 2.0 ** 10
+    # the other page's keys: scores of -72 * 8.125 / 8, -105.5 in log2 units (every number exact in its type)
+    q0 = 8.125
+    pool.kc[9, 0, :, 0] = ok.e4m3_code(-72.0)
+    q = np.zeros((1, 2, hd))
+    q[..., 0] = q0
+    for order in ([0, 1, 2, 3, 4, 5, 6, 7, 9], [9, 1, 2, 3, 4, 5, 6, 7, 8]):        # a wave takes every eighth of the keys' tiles
+        table = np.array([order], dtype=np.int32)
+        qt = dev(q, torch.float32).to(dtype)
+        o = bd_().kv_attention(pool.cache(), qt, dev(table), dev([0, 1]), dev([287]), dev([288]), 1)
+        ref, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q, table, [0, 1], [287], [288], 1)
+        assert (np.abs(host(o) - ref) <= attn_bound(ref, mag, big, hd, 288, dtype)).all(), order
