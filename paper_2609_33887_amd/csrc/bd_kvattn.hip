@@ -617,8 +617,10 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
 #pragma unroll
       for (int k = 0; k < KW; ++k) l += xs[k][qw][2][lane] * __builtin_amdgcn_exp2f(xs[k][qw][0][lane] - m_ref);
     }
-    // o = O 2^(r - m) / l; a query that sees nothing gives zeros
-    const float norm = (mx != -INFINITY ? 1.0f / l : l != l ? l : 0.f) * __builtin_amdgcn_exp2f(r_ref - m_ref);
+    // o = O 2^(r - m) / l; a query that sees nothing gives zeros.  2^(r - m) may lie below
+    // the normal floats while o does not (r - m is the V scale's exponent less 9 to 15).
+    const float norm = mx != -INFINITY ? 1.0f / l : l != l ? l : 0.f;
+    const int up = (int)fminf(fmaxf(r_ref - m_ref, -400.f), 400.f);
     const size_t slot = ((size_t)wg * 2 + (t_lo == 0 ? 1 : 0)) * AQ + qw * 32 + q_lane;
 #pragma unroll
     for (int j = 0; j < KW; ++j)
@@ -640,7 +642,7 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) x[i] *= norm;
+        for (int i = 0; i < R; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i] * norm, up);
         // register 16 d + 4 m + i (i < 4): dim 32 d + 8 m + 4 h + i of the lane's query
 #pragma unroll
         for (int i = 0; i < R; i += 4) {

@@ -73,3 +73,17 @@ def test_small_weights_of_pages_of_far_larger_values(dtype):
         o = bd_().kv_attention(pool.cache(), qt, dev(table), dev([0, 1]), dev([287]), dev([288]), 1)
         ref, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q, table, [0, 1], [287], [288], 1)
         assert (np.abs(host(o) - ref) <= attn_bound(ref, mag, big, hd, 288, dtype)).all(), order
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hd,lens", [(64, [3]), (128, [70, 33]), (128, [5000])])
+def test_values_of_the_smallest_scales(hd, lens, dtype):
+    """Pages whose V scale is far below what an exponential of float32 reaches from the weights' reference (2^-126)."""
+    pool = Pool(350 + hd + len(lens), sum(-(-x // 32) for x in lens) + 1, 2, hd, 32)
+    for E in (-126, -120, -113, 119):
+        pool.vs[:] = 2.0 ** E
+        got, ref, bound = run_attention(pool, lens, [1] * len(lens), 1, 4, dtype, workspace=True)
+        # below the type's normal numbers a rounding is half of its smallest one
+        bound = bound + 0.5 * torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+        assert (np.abs(got - ref) <= bound).all(), (E, np.max(np.abs(got - ref) / bound))
+        assert (got != 0).any()
