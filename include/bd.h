@@ -468,8 +468,9 @@ bd_status bd_kv_read(const bd_kv_cache* cache, void* k_dev, void* v_dev, int32_t
  *  query does not see have no effect on it, whatever their codes.
  *  scale: factor of the scores, > 0; 0 takes 1 / sqrt(head_dim).  Scores, softmax
  *  and sums are held in float32 and rounded once to dtype; queries are used with
- *  all their bits.  (A weight times its page's V scale is held to 2^-22 of itself
- *  or 2^-33 of the row's largest, whichever is more.)
+ *  all their bits; their products with K's codes are summed before the scales, so
+ *  head_dim 448 |q| has to stay below 2^128.  (A weight times its page's V scale is
+ *  held to 2^-22 of itself or 2^-33 of the row's largest, whichever is more.)
  *  max_rows: about the most rows a request has, 0 if unknown (chooses the kernel's
  *  form; results are right for any value).
  *  ws_dev, ws_bytes: workspace of bd_kv_attention_workspace bytes, 256-byte

@@ -397,7 +397,7 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
       u32x4 vb[BT][NY];
       floatx16_k a[BT];
       float sc[BT], ev[BT];
-      bool part = false;
+      bool part = false, odd = false;
 #pragma unroll
       for (int b = 0; b < BT; ++b) {
         const uint8_t* kp = sg.b[kw][b] + lane * 16;
@@ -417,12 +417,24 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
             for (int p = NQ - 1; p >= 0; --p)
               a[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[2 * y + e][p], a[b], 0, 0, 0);
           }
-        sc[b] = fmaxf(g.scale_log2 * sk, 0x1p-126f);
+        // one factor for the tile, unless it leaves the positive normal floats (below)
+        sc[b] = g.scale_log2 * sk;
+        odd |= __any(__builtin_amdgcn_classf(sc[b], 0x2FF));
         ev[b] = (float)scale_exponent(sv);
         part |= tl.t[b] * KT + KT > qend_lo;                   // some query does not see all of the tile
       }
       bool bad = false;
-      if (part) {
+      if (part || odd) {
+        // keys of the smallest scales, or a scale argument far from 1: the argument goes to
+        // the scores at once (as a branch of its own this check took 4 % of a long call)
+        if (odd) {
+#pragma unroll
+          for (int b = 0; b < BT; ++b) {
+            const float sk = sg.sc[wave][b][0][lane];
+            a[b] *= g.scale_log2;
+            sc[b] = fmaxf(sk, 0x1p-126f);
+          }
+        }
 #pragma unroll
         for (int b = 0; b < BT; ++b) {
 #pragma unroll
@@ -522,7 +534,7 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
             for (int p = 1; p >= 0; --p)
               oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[b][x][p], oacc[d], 0, 0, 0);
           }
-      if (part && __any(bad)) {
+      if ((part || odd) && __any(bad)) {
 #pragma unroll 1
         for (int b = 0; b < BT; ++b) {
           const int k0 = (b ? tl.t[BT - 1] : tl.t[0]) * KT;

@@ -87,3 +87,23 @@ def test_values_of_the_smallest_scales(hd, lens, dtype):
         bound = bound + 0.5 * torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
         assert (np.abs(got - ref) <= bound).all(), (E, np.max(np.abs(got - ref) / bound))
         assert (got != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ks,q0,scale", [(-126, 118, 0.0), (-100, 116, 2.0 ** -40), (28, -126, 2.0 ** 100), (-20, -80, 2.0 ** 100)])
+def test_scores_where_scale_times_page_scale_leaves_float32(ks, q0, scale, dtype):
+    """The product of the scores' factor and a page's K scale under 2^-126 or past 2^128, while the scores are ordinary ones; a
+    query of zeros beside the others."""
+    hd, T = 64, 32
+    pool = Pool(360, 4, 1, hd, T)
+    pool.ks[:] = 2.0 ** ks
+    table = np.array([[2, 0, 3]], dtype=np.int32)
+    q = np.zeros((2, 3, hd))
+    q[:, 0, 0], q[:, 1, 0], q[:, 1, 5] = 2.0 ** q0, -2.0 ** q0, 2.0 ** q0
+    pool.vc[2, 0, 4, 9] = 0x7F                                                      # a NaN that every query sees
+    o = bd_().kv_attention(pool.cache(), dev(q, torch.float32).to(dtype), dev(table), dev([0, 2]), dev([75]), dev([77]), 1, scale=scale)
+    ref, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q, table, [0, 2], [75], [77], 1, scale=scale or None)
+    bound = attn_bound(ref, mag, big, hd, 77, dtype)
+    bad = np.isnan(ref)
+    assert bad.sum() == 6 and (np.isnan(host(o)) == bad).all()
+    assert (np.abs(host(o) - ref)[~bad] <= bound[~bad]).all(), np.nanmax(np.abs(host(o) - ref) / bound)
