@@ -139,7 +139,7 @@ __global__ __launch_bounds__(PG_NT) void k_kv_pages(PageArgs a) {
 // while others would read it.
 hipError_t launch_kv_pages(const PageArgs& a, hipStream_t st) {
   if (a.n < 1 || a.n > KV_MAX_SEQS) return hipErrorInvalidValue;
-  const int wgs = a.info == a.free_count ? 0 : (a.rows_cap + PG_NT - 1) / PG_NT;
+  const int wgs = a.info == a.free_count ? 0 : (int)(((int64_t)a.rows_cap + PG_NT - 1) / PG_NT);
   k_kv_pages<<<1 + (wgs < 512 ? wgs : 512), PG_NT, 3 * (size_t)(a.n + 1) * sizeof(int), st>>>(a);
   return hipGetLastError();
 }
