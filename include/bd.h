@@ -378,9 +378,11 @@ bd_status bd_plan_projection(int32_t N, int32_t K, int32_t rows_cap, int32_t res
  * Calls over n requests take ragged rows: row_start_dev [n + 1] (ascending) gives
  * request s the rows [row_start[s], row_start[s + 1]) of the row buffers, and
  * pos0_dev [n] the position of its first row; row i of it is the token at
- * pos0[s] + i.  rows is the number of rows of the buffers; what lies outside
- * them, or outside the table, is left out.  Rows from row_start[n] on are not
- * touched.  dtype is BD_F32 or BD_BF16; row strides (ldk, ldv, ldq, ldo) are in
+ * pos0[s] + i.  rows is the number of rows of the buffers; rows behind them, and
+ * tokens behind the table, are left out (not stored; rows that bd_kv_read leaves as
+ * they were).  A request whose row_start[s] is negative is left out whole, as is one
+ * with a negative pos0[s] by bd_kv_store and bd_kv_read.  Rows from row_start[n] on
+ * are not touched.  dtype is BD_F32 or BD_BF16; row strides (ldk, ldv, ldq, ldo) are in
  * elements, at least a row's width, multiples of 16 bytes, and row buffers are
  * 16-byte aligned.  All of these calls are asynchronous on stream (NULL =
  * default), use the current device, allocate nothing and can be captured into a

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import kv as ok
-from tests.test_gpu_kv import DEV, Pool, bd_, dev, host, run_attention
+from tests.test_gpu_kv import DEV, Pool, attn_bound, bd_, dev, host
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +26,31 @@ def test_pages_with_the_largest_slot_map():
     assert host(info).tolist() == [6, 40, 0, 2] and host(table).tolist() == [[7, 6]]
     assert host(slot[:40]).tolist() == [7 * 32 + i for i in range(32)] + [6 * 32 + i for i in range(8)]
     assert host(i32[cap:cap + 40]).tolist() == list(range(40)) and int(i32[40]) == -5 and int(slot[40]) == -6
+
+
+def test_requests_that_are_left_out():
+    """A negative first row or position leaves the request out, whatever its other rows; the requests beside it are served."""
+    bd = bd_()
+    H, hd, T = 2, 64, 32
+    pool = Pool(370, 8, H, hd, T)
+    cache = pool.cache()
+    table = np.array([[0, 1], [2, 3], [4, 5]], dtype=np.int32)
+    x = dev(pool.rng.standard_normal((50, H, hd)), torch.float32)
+    before = [host(t) for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    for start, pos0 in (([-4, 20, 20, 20], [0, 0, 0]), ([0, 20, 20, 20], [-5, 0, 0])):
+        bd.kv_store(cache, x, x, dev(table), dev(start), dev(pos0))
+        assert all((a == host(t)).all() for a, t in zip(before, (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+        out = torch.full_like(x, 3.0)
+        bd.kv_read(cache, dev(table), dev(start), dev(pos0), out, out.clone())
+        assert (host(out) == 3.0).all()
+    start, pos0 = [-3, 20, 30, 50], [0, -2, 40]
+    out, q = torch.full_like(x, 3.0), dev(pool.rng.standard_normal((50, 4, hd)), torch.float32)
+    bd.kv_read(cache, dev(table), dev(start), dev(pos0), out, torch.empty_like(out))
+    want, _ = ok.cached(pool.kc, pool.ks, table[2], 60)
+    assert (host(out)[:30] == 3.0).all() and (host(out)[30:] == want[40:]).all()
+    # the attention serves rows at positions from 0 on; rows before them are zeros
+    o = bd.kv_attention(cache, q, dev(table), dev(start), dev(pos0), dev([64, 64, 60]), 1, out=torch.full_like(q, 3.0))
+    ref, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, host(q), table, [20, 20, 30, 50], pos0, [64, 64, 60], 1)
+    bound = attn_bound(ref, mag, big, hd, 64, torch.float32)
+    assert (host(o)[:20] == 3.0).all() and (host(o)[20:22] == 0).all()
+    assert (np.abs(host(o) - ref)[20:] <= bound[20:]).all() and (host(o)[22:] != 0).any()
