@@ -193,7 +193,9 @@ bd_status bd_quantize_mxfp4(const void* w_dev, int32_t rows, int32_t cols, int32
  *  BD_KV_PAIR (the default): in the precision of the activations, 16 significant
  *  bits of a bf16 model.  BD_KV_FP8 (bf16 models only): in 8-bit pages of
  *  page_size tokens (see bd_kv_store: one power-of-two scale for each page and kv
- *  head), a quarter of the memory.  A window's K and V are coded as they are
+ *  head), a quarter of the cache's memory.  (A forward's K and V rows wait for their
+ *  codes in the FFN's buffers; a model of ffn_dim, or top_k times d_model for experts,
+ *  below 2 n_kv_heads head_dim has 8 bytes more for each of their elements.)  A window's K and V are coded as they are
  *  written, every step anew, and attention reads the code values, of the prompt and
  *  of the window alike; a page that holds committed tokens in front of the window
  *  keeps the largest scale that it has had.  page_size is ignored for BD_KV_PAIR.

@@ -162,7 +162,7 @@ struct bd_state {
   int page = 0, kv_pages = 0, kv_cols = 0;
   uint8_t *k8, *v8;      // [layer][kv_pages][Hkv][page * hd]
   float *k8s, *v8s;      // [layer][kv_pages][Hkv]
-  float *krows, *vrows;  // [rows_cap][Hkv][hd]
+  float *krows, *vrows;  // [rows_cap][Hkv][hd], in the FFN's buffers where they fit
   int32_t *kv_table, *kv_free, *kv_misc;   // [b][kv_cols]; [kv_pages]; lengths, count, sums (see state_init)
   void* kv_ws;
   size_t kv_ws_bytes;
@@ -924,6 +924,10 @@ static bd_status state_layout(const bd_model* m, int32_t b, int32_t P, int32_t G
   ALLOC(s->parg, (size_t)ntiles * s->lm_cap * 4);
   ALLOC(s->conf, (size_t)s->lm_cap * 4);
   ALLOC(s->tok, (size_t)s->lm_cap * 4);
+  // An 8-bit cache's K and V rows on their way to the codes: from the QKV product to the
+  // store nothing is held by the FFN's buffers, the dense FFN's or the experts' outputs,
+  // which take them where their rows are long enough.
+  const int spare_rows = c.n_experts > 0 ? c.top_k * d : c.ffn_dim;
   // fp32 values or 2 bf16 planes: 4 bytes per element either way
   s->vstride = m->bf16 ? round_up(s->maxpos, 64) : s->maxpos;
   s->page = m->kv_fp8_page;
@@ -935,8 +939,7 @@ static bd_status state_layout(const bd_model* m, int32_t b, int32_t P, int32_t G
     ALLOC(s->v8, codes);
     ALLOC(s->k8s, scales * 4);
     ALLOC(s->v8s, scales * 4);
-    ALLOC(s->krows, (size_t)s->rows_cap * Hkv * hd * 4);
-    ALLOC(s->vrows, (size_t)s->rows_cap * Hkv * hd * 4);
+    if (2 * Hkv * hd > spare_rows) ALLOC(s->krows, (size_t)s->rows_cap * 2 * Hkv * hd * 4);
     ALLOC(s->kv_table, (size_t)s->kv_pages * 4);
     ALLOC(s->kv_free, (size_t)s->kv_pages * 4);
     ALLOC(s->kv_misc, ((size_t)3 * b + 8) * 4);
@@ -975,6 +978,10 @@ static bd_status state_layout(const bd_model* m, int32_t b, int32_t P, int32_t G
     ALLOC(s->act_sorted, s->act_bytes);
     s->pl_act = assign_cap * Fe;
     ALLOC(s->y_sorted, assign_cap * d * 4);
+  }
+  if (s->page) {
+    if (2 * Hkv * hd <= spare_rows) s->krows = c.n_experts > 0 ? s->y_sorted : (float*)s->Hact;
+    s->vrows = s->krows + (size_t)s->rows_cap * Hkv * hd;
   }
   s->attn_splits = m->bf16 && !s->page ? attention_splits(b, nb * B, H, Hkv, s->maxpos) : 1;
   if (s->attn_splits > 1) {

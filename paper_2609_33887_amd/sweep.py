@@ -113,12 +113,18 @@ def cache_bytes(w, kv=None, page: int = 32) -> int:
     """K/V cache memory of one batch of a bf16 model as the library holds it:
     bf16 pairs (4 bytes a value; V's positions rounded up to 64) or, for "fp8",
     whole pages of 1-byte codes with a 4-byte scale for each kv head and page,
-    K and V apart."""
+    K and V apart, and the fp32 rows of a forward before they are coded where the
+    FFN's buffers do not hold them.  Workspaces of the attention, which either
+    cache has, are not counted."""
     pos = w.prompt_len + w.gen_len
     rows = w.n_layers * w.batch * w.n_kv_heads
     if kv == "fp8":
         pages = -(-pos // page)
-        return 2 * rows * pages * (page * w.head_dim + 4)
+        width = 2 * w.n_kv_heads * w.head_dim
+        fits = width <= (w.top_k * w.d_model if w.n_experts else w.ffn_dim)
+        most = max(2 * w.n_inflight * w.block_size, w.prompt_len) * w.batch
+        staged = 0 if fits else 4 * width * (-(-most // 256) * 256)
+        return 2 * rows * pages * (page * w.head_dim + 4) + staged
     return 4 * rows * w.head_dim * (pos + -(-pos // 64) * 64)
 
 

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import kv as ok
-from tests.test_gpu_kv import DEV, Pool, attn_bound, bd_, dev, host
+from tests.test_gpu_kv import DEV, Pool, attn_bound, bd_, dev, host, small_model
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +54,28 @@ def test_requests_that_are_left_out():
     bound = attn_bound(ref, mag, big, hd, 64, torch.float32)
     assert (host(o)[:20] == 3.0).all() and (host(o)[20:22] == 0).all()
     assert (np.abs(host(o) - ref)[20:] <= bound[20:]).all() and (host(o)[22:] != 0).any()
+
+
+@pytest.mark.parametrize("kw", [{}, dict(n_experts=8, top_k=2, expert_ffn=128, n_shared=1, ffn_dim=0)])
+def test_memory_of_states(kw):
+    """What a state of 8-bit pages takes less than one of pairs is what the sweep counts, workspaces of either left out (and
+    the caches' memory is a quarter: the rows before they are coded take none of their own)."""
+    from paper_2609_33887_amd.sweep import cache_bytes
+    bd = bd_()
+    w, ws, prompts = small_model(n_layers=4, d_model=512, n_heads=8, n_kv_heads=4, head_dim=128, batch=8, prompt_len=2048, gen_len=64,
+                                 **dict(dict(ffn_dim=1024), **kw))
+    took = {}
+    for kv in (None, "fp8"):
+        m = bd.Model(w, ws, DEV, kv=kv)
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info(DEV)[0]
+        st = bd.State(m, prompts, w.gen_len, 0.9, 2, 16)
+        torch.cuda.synchronize()
+        took[kv] = free - torch.cuda.mem_get_info(DEV)[0]
+        st.close()
+        m.close()
+    want = cache_bytes(w) - cache_bytes(w, "fp8")
+    work = bd.bd_kv_attention_workspace(8, 4, 128, 8, 512, 32, 32, 66)
+    # a buffer's slack of 64 KB each, allocations in 2 MB
+    assert want - work - (4 << 20) <= took[None] - took["fp8"] <= want + (24 << 20), (took, want, work)
+    assert 3.9 * cache_bytes(w, "fp8") <= cache_bytes(w)
