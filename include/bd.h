@@ -322,9 +322,9 @@ bd_status bd_state_steps(const bd_state* st, int32_t* steps_out);
  */
 bd_status bd_state_stats(bd_model* model, bd_state* st, int64_t* out, int32_t n);
 
-/* Kernel classes timed by bd_profile / bd_profile_read.  BD_PROF_ROPE keeps its
- * number and stays zero: RoPE and the K/V cache write are part of the QKV product
- * (BD_PROF_GEMM_QKV). */
+/* Kernel classes timed by bd_profile / bd_profile_read.  BD_PROF_ROPE counts the
+ * coding of K and V into 8-bit pages, and stays zero without them: RoPE and the
+ * write of the pair cache are part of the QKV product (BD_PROF_GEMM_QKV). */
 enum {
     BD_PROF_EMBED = 0, BD_PROF_NORM = 1, BD_PROF_GEMM_QKV = 2, BD_PROF_ROPE = 3, BD_PROF_ATTN = 4,
     BD_PROF_GEMM_O = 5, BD_PROF_GEMM_GU = 6, BD_PROF_GEMM_DOWN = 7, BD_PROF_LM_HEAD = 8,

@@ -705,7 +705,7 @@ static bd_status run_forward(bd_model* m, bd_state* s, const PlanView& plan, int
                          s->kv_pages,       Hkv,               hd,                  s->page};
       KvAttnArgs at{};
       at.a = KvRows{plan.seq_row_start, plan.seq_win_len, plan.seq_win_start, s->kv_table, s->b, s->kv_cols, rows_cap};
-      LAUNCH(BD_PROF_ATTN, launch_kv_store(pool, at.a, false, s->krows, s->vrows, (int64_t)Hkv * hd, (int64_t)Hkv * hd, st));
+      LAUNCH(BD_PROF_ROPE, launch_kv_store(pool, at.a, false, s->krows, s->vrows, (int64_t)Hkv * hd, (int64_t)Hkv * hd, st));
       if (kv_only) break;
       at.q = s->Qb;
       at.out = s->Ob;

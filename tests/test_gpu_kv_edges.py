@@ -79,3 +79,22 @@ def test_memory_of_states(kw):
     # a buffer's slack of 64 KB each, allocations in 2 MB
     assert want - work - (4 << 20) <= took[None] - took["fp8"] <= want + (24 << 20), (took, want, work)
     assert 3.9 * cache_bytes(w, "fp8") <= cache_bytes(w)
+
+
+def test_profile_classes_of_a_coded_decode():
+    """The attention class holds one launch a layer and step (the prompt's last layer has none), whichever the cache; the
+    coding of K and V has a class of its own."""
+    bd = bd_()
+    w, ws, prompts = small_model()
+    for kv in (None, "fp8"):
+        m = bd.Model(w, ws, DEV, kv=kv)
+        bd.bd_profile(m.handle, True)
+        st = bd.State(m, prompts, w.gen_len, 0.9, 2, 16)
+        for _ in range(3):
+            st.step()
+            st.commit()
+        prof = bd.bd_profile_read(m.handle)
+        st.close()
+        m.close()
+        assert prof["attn"][1] == 2 * 3 + 1 and prof["gemm_qkv"][1] == 2 * 4, prof
+        assert prof["rope"][1] == (2 * 4 if kv else 0) and (prof["rope"][0] > 0) == bool(kv), prof
