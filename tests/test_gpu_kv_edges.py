@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from oracle import kv as ok
-from tests.test_gpu_kv import DEV, Pool, attn_bound, bd_, dev, host, small_model
+from tests.test_gpu_kv import DEV, Pool, attn_bound, bd_, dev, host, run_attention, small_model
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +98,23 @@ def test_profile_classes_of_a_coded_decode():
         m.close()
         assert prof["attn"][1] == 2 * 3 + 1 and prof["gemm_qkv"][1] == 2 * 4, prof
         assert prof["rope"][1] == (2 * 4 if kv else 0) and (prof["rope"][0] > 0) == bool(kv), prof
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_cut_keys_of_the_most_requests(hd, dtype):
+    """1024 requests, of which 40 have rows, one of them 5000 keys: the plan's sums over more requests than a workgroup has
+    threads, requests from number 256 on, the most local memory, keys cut into ranges."""
+    n, T = 1024, 32
+    rng = np.random.default_rng([73, hd])
+    at = [3, 255, 256, 511, 512, 1023] + sorted(rng.choice(np.arange(260, 1000), 34, replace=False).tolist())
+    cnt, lens = np.zeros(n, int), np.zeros(n, int)
+    cnt[at], lens[at] = rng.integers(1, 4, len(at)), rng.integers(4, 300, len(at))
+    lens[512], lens[256] = 5000, 1700
+    pool = Pool(380 + hd, 200, 1, hd, T)
+    table = rng.integers(0, 200, (n, -(-5000 // T) + 1)).astype(np.int32)           # pages shared, as read-only ones may be
+    R = int(cnt.sum()) + 2                                                           # the rows that run_attention passes
+    assert bd_().bd_kv_attention_workspace(4, 1, hd, n, R, int(cnt.max()), T, table.shape[1]) > 0
+    for ws in (True, False):
+        got, ref, bound = run_attention(pool, lens, cnt, 1, 4, dtype, table=table, workspace=ws)
+        assert (np.abs(got - ref) <= bound).all() and (got != 0).any(axis=(1, 2)).all()

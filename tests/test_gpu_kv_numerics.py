@@ -20,14 +20,15 @@ def computed_bound(ref, mag, big, hd, keys):
     return attn_bound(ref, mag, big, hd, keys, torch.float32)
 
 
-FORMS = [([1057], [1], 16, 4, 128, 32, 1, 0),                                       # eight waves a query group
-         ([1057], [1], 16, 16, 64, 32, 1, 0),
-         ([9000, 40], [1, 5], 16, 4, 128, 64, 1, 0),                                # keys cut into ranges
-         ([1440] * 3, [96] * 3, 16, 4, 128, 32, 32, 64),                            # two query groups, by the hint
-         ([700] * 3, [96] * 3, 8, 2, 64, 32, 32, 16),
-         ([1100, 640, 900, 400], [1000, 640, 900, 77], 16, 8, 128, 64, 32, 0),      # four
-         ([900, 1100], [900, 1100], 16, 16, 64, 32, 1, 0),
-         ([2500] * 2, [64] * 2, 16, 4, 128, 32, 64, 1000)]
+# lengths, rows, q-heads, kv-heads, head size, page, block, columns of the table behind the longest request (the kernel's
+# form goes by the table and the rows): one query group of eight waves, whole and with its keys cut into ranges; two groups;
+# four
+FORMS = [([1057], [1], 16, 4, 128, 32, 1, 2), ([1057], [1], 16, 16, 64, 32, 1, 2), ([1440] * 3, [96] * 3, 16, 4, 128, 32, 32, 2),
+         ([9000, 40], [1, 5], 16, 4, 128, 64, 1, 2), ([2500] * 2, [64] * 2, 16, 4, 128, 32, 64, 2),
+         ([300] * 6, [96] * 6, 16, 16, 64, 32, 32, 2), ([1100, 640, 900, 400], [400, 640, 300, 77], 16, 8, 128, 64, 32, 2),
+         ([2100] + [200] * 5, [96] * 6, 16, 16, 64, 32, 32, 2),
+         ([700, 640, 700, 400], [700, 640, 700, 77], 16, 8, 128, 64, 32, 2), ([1500] + [130] * 5, [96] * 6, 16, 16, 64, 32, 32, 256),
+         ([1500] + [130] * 5, [96] * 6, 16, 16, 128, 32, 32, 256)]
 
 
 @pytest.mark.parametrize("i", range(len(FORMS)))
@@ -38,10 +39,10 @@ def test_bf16_outputs_are_the_rounded_float64_ones(i):
     (sums of hd terms: sqrt(hd) 2^-24 of a size of about 5, then 2^-22 of v_exp_f32) leave weights off by some 1e-6 and
     an output by 3e-6 at most, each key's error its own: 2 * 3e-6 of a step of 2^-8 is a share of 1.5e-3 moved by 2^-7 of
     themselves at most, sqrt(1.5e-3) 2^-7 = 3e-4 of the norm."""
-    lens, cnt, H, Hkv, hd, T, B, max_rows = FORMS[i]
+    lens, cnt, H, Hkv, hd, T, B, spare = FORMS[i]
     pool = Pool(300 + i, sum(-(-x // T) for x in lens) + 2, Hkv, hd, T, spread=1)
-    table = pool.tables(lens)
-    got, ref, _ = run_attention(pool, lens, cnt, B, H, torch.bfloat16, seed=i, table=table, max_rows=max_rows)
+    table = pool.tables(lens, spare)
+    got, ref, _ = run_attention(pool, lens, cnt, B, H, torch.bfloat16, seed=i, table=table)
     q = np.random.default_rng([5, i]).standard_normal((sum(cnt), H, hd))
     q = host(dev(q, torch.float32).to(torch.bfloat16))
     again, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q, table, starts(cnt), np.array(lens) - cnt, lens, B)
