@@ -135,8 +135,10 @@ def precision_sweep(w, models, prompts, G, B, reference, candidates, alpha, delt
     the cost measure is the weight-memory reduction against the reference
     (larger is better), so the deployed configuration is the valid one with
     the least weight memory (first listed among equals).  ``memory``: bytes of a
-    key of ``models`` in place of its weights'."""
-    if memory is None:
+    key of ``models`` in place of its weights'; the result's ``memory_bytes`` are
+    these, and it has ``weight_bytes`` where they are the weights'."""
+    weights = memory is None
+    if weights:
         memory = lambda prec: weight_bytes(w, None if prec == "bf16" else prec)
     grid = [tuple(reference)] + [tuple(c) for c in candidates]
     outs, tpf, mem = [], [], []
@@ -154,7 +156,7 @@ def precision_sweep(w, models, prompts, G, B, reference, candidates, alpha, delt
     cost = mem[0] / np.array(mem, dtype=np.float64)
     V, p, valid, sel = bd.rl_select(correct, cost, 0, alpha, delta, method)
     return {"grid": grid, "labels": [f"{prec}/{label(cfg)}" for prec, cfg in grid], "tpf": tpf,
-            "weight_bytes": mem, "cost": cost, "correct": correct, "V": V, "p": p, "valid": valid,
+            "memory_bytes": mem, **({"weight_bytes": mem} if weights else {}), "cost": cost, "correct": correct, "V": V, "p": p, "valid": valid,
             "selected": sel, "tokens": outs}
 
 
@@ -189,7 +191,8 @@ def main():
                             batch=w.batch, progress=say, method=args.method, memory=memory)
         print(json.dumps({"workload": w.name, "prompts": args.prompts, "alpha": args.alpha,
                           "delta": args.delta, "method": args.method, "grid": r["labels"], "tpf": r["tpf"],
-                          "cache_bytes" if args.grid == "kv" else "weight_bytes": r["weight_bytes"], "V": r["V"].tolist(), "p": r["p"].tolist(),
+                          "cache_bytes" if args.grid == "kv" else "weight_bytes": r["memory_bytes"],
+                          "V": r["V"].tolist(), "p": r["p"].tolist(),
                           "valid": r["valid"].tolist(), "selected": r["selected"],
                           "selected_config": r["labels"][r["selected"]]}))
         return

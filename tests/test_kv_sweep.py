@@ -19,3 +19,19 @@ def test_cache_bytes_count_the_rows_that_no_buffer_holds():
     assert cache_bytes(workload(**moe), "fp8") == coded
     assert cache_bytes(workload(**dict(moe, top_k=1)), "fp8") == coded + 256 * 512 * 4
     assert cache_bytes(workload(ffn_dim=384)) == cache_bytes(workload())
+
+
+def test_precision_sweep_names_what_it_counts(monkeypatch):
+    """Weight bytes only where the weights are what is compared; the least memory among the valid ones is deployed."""
+    import numpy as np
+    from paper_2609_33887_amd import sweep
+    toks = np.arange(40 * 60).reshape(40, 60)
+    monkeypatch.setattr(sweep, "decode_all", lambda model, prompts, G, cfg, B, batch: (toks, np.full(40, 12)))
+    w = workload()
+    run = lambda names, memory: sweep.precision_sweep(w, dict.fromkeys(names), None, 60, 4, (names[0], (0.9, 1)),
+                                                      [(names[1], (0.9, 1))], 0.1, 0.1, memory=memory)
+    r = run(("pair", "kv-fp8"), lambda p: sweep.cache_bytes(w, "fp8" if p == "kv-fp8" else None))
+    assert "weight_bytes" not in r and r["memory_bytes"] == [sweep.cache_bytes(w), sweep.cache_bytes(w, "fp8")]
+    assert r["selected"] == 1
+    r = run(("bf16", "fp8"), None)
+    assert r["weight_bytes"] == r["memory_bytes"] == [sweep.weight_bytes(w), sweep.weight_bytes(w, "fp8")]
