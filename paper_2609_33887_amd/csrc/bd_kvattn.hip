@@ -199,7 +199,7 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
   constexpr int NQ = AttnMode<MODE>::NQ, NY = HD / 32, NT = 64 * QW * KW, AQ = 32 * QW;
   constexpr int LPW = 2 * NY / QW;             // 1 KiB loads a wave issues for a tile
   constexpr int LPS = BT * (LPW + 2);          // loads of a stage, its scales among them
-  constexpr int D = KW == 8 && HD == 128 ? 2 : 3;   // stages of the ring: 128 KB, else 96 KB at most
+  constexpr int D = KW == 8 && HD == 128 ? 2 : 3;   // stages of the ring: 136 KB, else 108 KB at most
   static_assert(LPW * QW == 2 * NY && LPS < 64, "whole loads");
   constexpr int A_SLOTS = attn_slots(KW);
   typedef KvStage<HD, QW, KW, BT> Stage;
@@ -210,6 +210,9 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
   __shared__ float fw[NT / 64];
   __shared__ int iw[NT / 64][2];
   __shared__ float xs[KW][QW][3][64];
+  // (151 KB of 160 in the largest form, with 10 of the most requests)
+  static_assert(D * sizeof(Stage) + sizeof(xs) + sizeof(tmp) + sizeof(fw) + sizeof(iw) + KV_ATTN_SEQS * sizeof(int) +
+                A_HELD * sizeof(AttnSeq) <= 160 * 1024, "the local memory of a CU");
   const int G = g.H / c.Hkv, n = g.a.n, tid = threadIdx.x;
   // ---- plan
   AttnSeq mine{};
