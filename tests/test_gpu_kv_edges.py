@@ -118,3 +118,24 @@ def test_cut_keys_of_the_most_requests(hd, dtype):
     for ws in (True, False):
         got, ref, bound = run_attention(pool, lens, cnt, 1, 4, dtype, table=table, workspace=ws)
         assert (np.abs(got - ref) <= bound).all() and (got != 0).any(axis=(1, 2)).all()
+
+
+@pytest.mark.parametrize("page", [32, 96])
+def test_coded_decode_without_a_prompt(page):
+    """No prompt at all: the window's own tokens are the cache's first, step by step against the float64 oracle with the same
+    codes.  (Tolerances of one layer, derived in test_gpu_kv.py.)"""
+    import tests.gpu_harness as gh
+    from oracle.model import OracleModel
+    bd = bd_()
+    w, ws, prompts = small_model(n_layers=1)
+    none = np.ascontiguousarray(prompts[:, :0])
+    m = bd.Model(w, ws, DEV, kv="fp8", kv_page=page)
+    tr = gh.capture_gpu_trace(m, none, w.gen_len, 0.9, 2, w.block_size, logits_for={0})
+    rep = gh.lockstep(ok.with_coded_cache(OracleModel(w, ws, "f64"), page), none, [0], tr, w.gen_len, 0.9, 2, w.block_size, 5e-3, 3e-2)
+    a, b = (bd.decode(m, none, w.gen_len, 0.9, 2, w.block_size) for _ in range(2))
+    st = bd.State(m, none, w.gen_len, 0.9, 2, w.block_size)
+    st.reset()                                                                       # (a prompt of no tokens ends at a page's end)
+    st.close()
+    m.close()
+    assert all((x == y).all() for x, y in zip(a, b))
+    assert not rep.failures and rep.complete, rep
