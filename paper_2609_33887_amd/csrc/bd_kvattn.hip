@@ -17,19 +17,21 @@
 // The products take w as two fp16 parts: 22 bits, or 2^-33 of the row's largest w
 // where that is more (one part, 11 bits, moved one bf16 output in thirty to its
 // neighbour, 8e-4 of the outputs' norm against 5e-5; 8 windows of 128 rows over
-// 8320 keys took 113 us and take 133).  Queries are one, two or three bf16 planes
+// 8320 keys took 103 us and take 129).  Queries are one, two or three bf16 planes
 // (bf16, the models' pairs, fp32: exact).  Sums are fp32.
 //
 // What bounds it.  Single tokens read every code once: 48 requests of very unequal
-// lengths, 0.80 GB in 163 us, 4.9 TB/s (a copy moves 5.2).  With 100 queries or
-// more a (request, kv head) it is the issue of vector instructions: a bf16 wave's
-// tile takes 16 matrix instructions (0.27 us) and about 172 vector ones (0.40 us),
-// 64 of them conversions of the codes, and two waves a SIMD take 0.41 us a tile
-// each: 8 windows of 128 rows over 8320 keys, 70 GFLOP in 102 us, 0.68 PFLOP/s
-// (a library product of 8192^3 makes 1.2).  (The scaled fp8 matrix instruction
-// would take K's codes as they are, but its sums of 64 products are off by 1.5e-4 of
-// their magnitudes.)  Short calls are a chain of loads: plan, table, tiles, join, 9 us
-// for one token over 33 keys.
+// lengths, 0.80 GB in 166 us, 4.8 TB/s (a copy moves 5.2).  With 100 queries or
+// more a (request, kv head) it is the sum of matrix and vector instructions, which do
+// not overlap: a stage forms all its scores, then the weights, then the outputs.  A
+// bf16 wave's tile takes 24 matrix instructions of 32 cycles and 199 vector ones, 64 of
+// them conversions of the codes: 8 windows of 128 rows over 8320 keys, 70 GFLOP in
+// 129 us, 0.54 PFLOP/s (a library product of 8192^3 makes 1.2), 130 such tiles a SIMD
+// in 242,000 cycles, of which vector instructions are issued in 52 % and the matrix
+// units busy in 41 %.  (The scaled fp8 matrix instruction would take K's codes as they
+// are, but its sums of 64 products are off by 1.5e-4 of their magnitudes.)  Calls over
+// few, unlike units take as long as the longest.  Short calls are a chain of loads:
+// plan, table, tiles, 10 us for one token over 33 keys.
 #include "bd_kv.h"
 
 namespace bd {
@@ -156,12 +158,13 @@ __host__ __device__ inline AttnWs attn_ws(void* ws, int wgs, int AQ) {
 }
 
 // Workgroups that the card runs at once (two of four waves a CU, or one of eight),
-// over which the keys of fewer units are dealt (8 windows of 128 rows over 8320 keys
-// 112 us, over 256 of four waves 122); the fewest key tiles dealt to one (single tokens
-// with 2 / 4 / 8 tiles a wave: one over 4096 keys 15 / 17 / 22, over 32768 32 / 24 / 25,
-// eight over up to 4096 22 / 24 / 34; a window of 96 rows over 4096 27 / 21 / 25); and the
-// tiles' time that a join costs, its partials' way through memory and the ranges that
-// begin and end inside units (24 windows of up to 1440 keys 42, cut at half the price 50).
+// over which the keys of fewer units are dealt (us of a replayed call: 8 windows of 128
+// rows over 8320 keys 136, over 256 of four waves 145); the fewest key tiles dealt to one
+// (single tokens with 2 / 4 / 8 tiles a wave: one over 4096 keys 16 / 19 / 24, over 32768
+// 34 / 26 / 29, eight over up to 4096 24 / 26 / 36; a window of 96 rows over 4096 28 / 23 /
+// 27); and the tiles' time that a join costs, its partials' way through memory and the
+// ranges that begin and end inside units (24 windows of up to 1440 keys 48, cut at half
+// the price 54).
 __host__ __device__ constexpr int attn_slots(int KW) { return KW == 8 ? 256 : 512; }
 // Waves over the keys for each number of query groups.
 __host__ __device__ constexpr int attn_kw(int QW) { return QW == 1 ? 8 : QW == 2 ? 2 : 1; }
@@ -175,7 +178,8 @@ constexpr int KVA_DWORD3 = 0x00020000;
 
 // One stage: BT tiles of keys for each of the KW waves of a query group, K then V (two
 // where one wave has a query group and registers for them, heads of 64 or bf16 queries:
-// 112 against 120 us for 8 windows over 8320 keys, but 195 against 174 in fp32),
+// 136 against 139 us for 8 windows over 8320 keys, fp32 prompts of heads of 64 49 against
+// 51, but those windows in fp32 201 against 174),
 // and for every wave its tiles' scales, each in 64 words alike.
 template <int HD, int QW, int KW, int BT>
 struct KvStage {
@@ -752,14 +756,14 @@ static size_t attn_form_bytes(int hd, int ranges, int AQ) {
 // reads every key tile for 32 queries only but is done soonest, and needs no join while
 // its units find a CU each: taken for 32 queries a (request, kv head) and where there
 // are at most 256 such units (us with 1 / 2 / 4 groups, q-heads in fours, 1440 keys:
-// one window of 96 rows 18 / 23 / 25, four 19 / 32 / 34, twelve 51 / 42 / 48).  Two groups
+// one window of 96 rows 19 / 23 / 26, four 21 / 34 / 38, twelve 55 / 48 / 53).  Two groups
 // with two waves each halve the time of the longest unit: for 64 queries, where all fit
 // the card at once, and with heads of 128 and tables of 1024 keys or more up to 1280 units
-// (32 ragged windows 73 / 56 / 63, 48 of them 110 / 62 / 66, 16 prompts of 512 in 2048
-// units 92 / 37 / 34, but 24 windows of 128 keys - / 19 / 16.5; of heads of 64 four groups
-// lose less: 6 prompts of 1023 in 920 units 83 / 39 / 36).  Unless the tables span so many
+// (32 ragged windows 78 / 66 / 69, 48 of them 116 / 72 / 80, 16 prompts of 512 in 2048
+// units 95 / 40 / 39, but 24 windows of 128 keys 48 / 20 / 18; of heads of 64 four groups
+// lose less: 6 prompts of 1023 in 920 units 87 / 43 / 41).  Unless the tables span so many
 // keys that the workgroups are busy for long: four groups take two tiles a stage, the
-// fastest loop (twelve windows over 8192 keys 157 / 129 / 116).
+// fastest loop (twelve windows over 8192 keys 187 / 158 / 146).
 static int attn_qw(int H, int Hkv, int hd, int n, int rows, int max_rows, int64_t keys) {
   const int64_t G = H / Hkv, q = G * (max_rows > 0 ? max_rows : (rows + n - 1) / n), kt = (keys + KT - 1) / KT;
   auto units = [&](int Q) {

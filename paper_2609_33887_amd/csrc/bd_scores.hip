@@ -409,10 +409,11 @@ __global__ __launch_bounds__(SC_NT) void k_scores_merge(ScoreArgs a, int segs) {
 
 // Segments of a row: about 1024 workgroups in all, four a CU, which read as fast as
 // more do, while every segment costs its own threshold, sorting and part of the join
-// (152064 logits in us, 1 / 2 / 4 / 8 / 16 segments: 2011 rows bf16 145 / 164 / 194 /
-// 253 / 376, 400 rows 66 / 61 / 60 / 70 / 96, 96 rows fp32 64 / 44 / 31 / 27 / 26, one
-// row 51 / 35 / 25 / 20 / 16); a wave keeps two steps of its own (24 rows of 32768: 4
-// segments 13.8, 8 12.7).
+// (us of replayed calls on the same 152064 logits a row, 1 / 2 / 4 / 8 / 16 segments: 2011
+// rows bf16 145 / 163 / 196 / 254 / 377, 400 rows 66 / 61 / 61 / 70 / 96, 96 rows fp32 65 /
+// 44 / 32 / 27 / 27, one row 52 / 36 / 25 / 20 / 16; among calls on other rows the first
+// takes the 132 above); a wave keeps two steps of its own (24 rows of 32768: 4 segments
+// 14.2, 8 13.0).
 static int score_segs(int rows, int V) {
   const int most = (V + 2 * SC_WAVES * SC_STEP - 1) / (2 * SC_WAVES * SC_STEP);
   int s = (int)((1024 + (int64_t)rows / 2) / rows);
