@@ -437,9 +437,9 @@ void k_kv_attn(KvPages c, KvAttnArgs g, int slots) {
         if (odd) {
 #pragma unroll
           for (int b = 0; b < BT; ++b) {
-            const float sk = sg.sc[wave][b][0][lane];
-            a[b] *= g.scale_log2;
-            sc[b] = fmaxf(sk, 0x1p-126f);
+            const bool out = __builtin_amdgcn_classf(sc[b], 0x2FF);
+            a[b] *= out ? g.scale_log2 : 1.f;
+            sc[b] = out ? fmaxf(sg.sc[wave][b][0][lane], 0x1p-126f) : sc[b];
           }
         }
 #pragma unroll

@@ -108,3 +108,28 @@ def test_scores_where_scale_times_page_scale_leaves_float32(ks, q0, scale, dtype
     bad = np.isnan(ref)
     assert bad.sum() == 6 and (np.isnan(host(o)) == bad).all()
     assert (np.abs(host(o) - ref)[~bad] <= bound[~bad]).all(), np.nanmax(np.abs(host(o) - ref) / bound)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_pages_beside_one_whose_factor_leaves_float32(dtype):
+    """One page at the lowest scale among ordinary ones (two tiles a stage in the form that many rows take), and a scale
+    argument so large that the ordinary pages' scores would leave float32 without their own scale."""
+    hd, T, n = 64, 32, 40
+    pool = Pool(365, 4, 16, hd, T)
+    pool.kc[:] = ok.e4m3_code(np.abs(pool.rng.standard_normal(pool.kc.shape)) * 60.0 + 1)
+    table = np.tile(np.array([[2, 0, 3]], dtype=np.int32), (n, 1))
+    q = np.zeros((100 * n, 16, hd))
+    q[..., 3] = 1.0
+    for scale, ks in ((0.0, (-3, -126, -3)), (2.0 ** 126, (-125, 10, -124))):
+        for p, e in zip(table[0], ks):
+            pool.ks[p] = 2.0 ** e
+        if scale:
+            pool.kc[0] = 0                                                          # its scores are 0, whatever its scale
+        qt = dev(q, torch.float32).to(dtype)
+        start = np.arange(n + 1) * 100
+        o = bd_().kv_attention(pool.cache(), qt, dev(table), dev(start), dev(np.zeros(n)), dev(np.full(n, 77)), 0, scale=scale, max_rows=100)
+        few = slice(0, 100)
+        ref, mag, big = ok.attention(pool.kc, pool.ks, pool.vc, pool.vs, q[few], table[:1], [0, 100], [0], [77], 0, scale=scale or None)
+        bound = attn_bound(ref, mag, big, hd, 77, dtype)
+        assert (np.abs(host(o[few]) - ref) <= bound).all(), np.max(np.abs(host(o[few]) - ref) / bound)
+        assert torch.equal(o.view(n, 100, 16, hd), o[:100].expand(n, 100, 16, hd))
